@@ -3,8 +3,8 @@
 // One CTA per row, or one warp where there are many short rows.  A thread keeps its entries of h = x + residual in registers as
 // f32 (8 per chunk, up to four chunks), so that x and the residual are read once and everything that follows (sum of squares, the
 // row's factor, the groups' largest entries, the codes) happens on chip: the kernel moves what it cannot do without and is bound
-// by HBM for many rows, by one chain of load - reduction - store latencies for few.  Measured: 8192 x 8192 bf16 to e4m3 86 us
-// (5.5 TB/s of the 6.5 that a copy reaches), 4096 x 4096 in f32 42.1 us (6.4 TB/s), 1 x 4096 3.5 us (a launch of an empty kernel
+// by HBM for many rows, by one chain of load - reduction - store latencies for few.  Measured: 8192 x 8192 bf16 to e4m3 87 us
+// (5.4 TB/s of the 6.5 that a copy reaches), 4096 x 4096 in f32 42.1 us (6.4 TB/s), 1 x 4096 3.5 us (a launch of an empty kernel
 // takes as long).
 //   wide    a thread's 8 entries are consecutive: one 16-byte load per 16-bit tensor; a group of 32 / 64 / 128 columns
 //           is 4 / 8 / 16 neighbouring lanes.
@@ -84,12 +84,45 @@ __device__ __forceinline__ void store8(T *p, const float (&v)[8]) {
     }
 }
 
-// 1 / m to the last bit or so (the hardware's approximation and a Newton step)
-__device__ __forceinline__ float reciprocal(float m) {
-    float r;
-    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(m));
-    return fmaf(fmaf(-m, r, 1.0f), r, r);
+// Two entries in one instruction: a = a * x, a = a * x + y (rounded as the single forms are)
+__device__ __forceinline__ void mul_pair(float &a, float &b, float x) {
+    asm("{\n\t.reg .b64 p, q;\n\tmov.b64 p, {%0, %1};\n\tmov.b64 q, {%2, %2};\n\tmul.rn.f32x2 p, p, q;\n\tmov.b64 {%0, %1}, p;\n\t}" : "+f"(a), "+f"(b) : "f"(x));
 }
+__device__ __forceinline__ void fma_pair(float &a, float &b, float x, float y, float z) {
+    asm("{\n\t.reg .b64 p, q, r;\n\tmov.b64 p, {%0, %1};\n\tmov.b64 q, {%2, %2};\n\tmov.b64 r, {%3, %4};\n\tfma.rn.f32x2 p, p, q, r;\n\tmov.b64 {%0, %1}, p;\n\t}"
+        : "+f"(a), "+f"(b) : "f"(x), "f"(y), "f"(z));
+}
+
+// Division by a number whose reciprocal is known to a unit or so: the product with it is at most three units off, the remainder of that is
+// exact in a fused multiply-add, and the remainder times the reciprocal, added, rounds the quotient once (Markstein, IBM J. Res. Dev. 34,
+// 1990): what IEEE division gives, unless the quotient lies within 2^-20 units of the middle of two f32 values.
+__device__ __forceinline__ float quotient(float y, float minus_s, float r) {
+    const float q = y * r;
+    return fmaf(fmaf(q, minus_s, y), r, q);
+}
+// Eight quotients at a time by one scale.  (8192 x 8192 with the division itself, entry by entry: 119 us.)
+struct Divisor {
+    float minus_s, r;
+    // 0: every quotient is 0.  An infinity: finite / it is 0, infinite / it NaN, both from the reciprocal alone.
+    __device__ __forceinline__ explicit Divisor(float s) : minus_s(fabsf(s) == INFINITY ? 0.0f : -s) {
+        asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(s));
+        if (s == 0.0f) r = 0.0f;
+    }
+    __device__ __forceinline__ void of(const float (&y)[8], float (&v)[8]) const {
+#pragma unroll
+        for (int j = 0; j < 8; j += 2) {
+            float a = y[j], b = y[j + 1];
+            mul_pair(a, b, r);
+            v[j] = a;
+            v[j + 1] = b;
+            fma_pair(a, b, minus_s, y[j], y[j + 1]);
+            fma_pair(a, b, r, v[j], v[j + 1]);
+            v[j] = a;
+            v[j + 1] = b;
+        }
+    }
+    __device__ __forceinline__ float of(float y) const { return quotient(y, minus_s, r); }
+};
 
 // codes of eight entries, two bytes at a time
 __device__ __forceinline__ uint2 codes_of(const float (&v)[8], int dtype) {
@@ -212,9 +245,8 @@ __global__ void __launch_bounds__(1024) rms_norm_kernel(NormArgs a) {
                 load_batch(a.weight, a.weight_dtype, [&](int j) { return min(k + 32 * j, a.cols - 1); }, w);
             }
         }
-        // (8 bits: the codes are entry / largest entry, from which the row's factor cancels; it goes into the scale alone)
 #pragma unroll
-        for (int j = 0; j < 8; ++j) h[c][j] = CODES ? h[c][j] * w[j] : h[c][j] * factor * w[j];
+        for (int j = 0; j < 8; ++j) h[c][j] = h[c][j] * factor * w[j];
     }
 
     if (!CODES) {
@@ -236,38 +268,40 @@ __global__ void __launch_bounds__(1024) rms_norm_kernel(NormArgs a) {
         return;
     }
 
-    const float q = a.out_dtype == MOM_E4M3 ? 448.0f : 127.0f, per_q = a.out_dtype == MOM_E4M3 ? 1.0f / 448.0f : 1.0f / 127.0f;
-    // 8 bits: largest entry of each group, scale = factor * largest / Q, codes = entry * (Q / largest); a NaN factor makes all of them NaN
-    auto scale_of = [&](float m) { const float v = m * factor; return v < SMALLEST ? 0.0f : v * per_q; };
-    auto inverse_of = [&](float m) { const float v = m * factor; return v < SMALLEST ? 0.0f : v == v ? q * reciprocal(m) : v; };
+    // 8 bits: scale = largest entry of the group / Q, codes = entry / scale
+    const float minus_q = a.out_dtype == MOM_E4M3 ? -448.0f : -127.0f, per_q = a.out_dtype == MOM_E4M3 ? 1.0f / 448.0f : 1.0f / 127.0f;
+    auto scale_of = [&](float m) { return m < SMALLEST ? 0.0f : m < INFINITY ? quotient(m, minus_q, per_q) : m; };
     float *scales = a.scales + row * a.groups;
     uint8_t *out = static_cast<uint8_t *>(a.out) + row * a.out_stride;
-    float row_max = 0.0f;
+    float row_scale = 0.0f;
     if (a.group == 0) {
+        float row_max = 0.0f;
 #pragma unroll
         for (int c = 0; c < CHUNKS; ++c)
 #pragma unroll
             for (int j = 0; j < 8; ++j) row_max = max_nan(row_max, fabsf(h[c][j]));
         row_max = row_reduce<true, WARP>(row_max, slots[1]);
-        if ((WARP ? lane : threadIdx.x) == 0) scales[0] = scale_of(row_max);
+        row_scale = scale_of(row_max);
+        if ((WARP ? lane : threadIdx.x) == 0) scales[0] = row_scale;
     }
+    const Divisor by_row(row_scale);
 #pragma unroll
     for (int c = 0; c < CHUNKS; ++c) {
         const int k = column(c, 0);
-        float inv[8];
+        float v[8];
         if (a.group == 0) {
-            const float v = inverse_of(row_max);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) inv[j] = v;
+            by_row.of(h[c], v);
         } else if (WIDE) {
             float m = 0.0f;
 #pragma unroll
             for (int j = 0; j < 8; ++j) m = max_nan(m, fabsf(h[c][j]));
-            for (int o = 1; o < a.group / 8; o <<= 1) m = max_nan(m, __shfl_xor_sync(~0u, m, o));
-            const float v = inverse_of(m);
-            if (k < a.cols && k % a.group == 0) scales[k / a.group] = scale_of(m);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) inv[j] = v;
+            m = max_nan(m, __shfl_xor_sync(~0u, m, 1));
+            m = max_nan(m, __shfl_xor_sync(~0u, m, 2));
+            if (a.group >= 64) m = max_nan(m, __shfl_xor_sync(~0u, m, 4));
+            if (a.group == 128) m = max_nan(m, __shfl_xor_sync(~0u, m, 8));
+            const float scale = scale_of(m);
+            if (k < a.cols && k % a.group == 0) scales[k / a.group] = scale;
+            Divisor(scale).of(h[c], v);
         } else {
             const int per = a.group / 32;                // 1, 2 or 4 columns of the lane share a scale
             float m[8];
@@ -281,24 +315,27 @@ __global__ void __launch_bounds__(1024) rms_norm_kernel(NormArgs a) {
 #pragma unroll
                 for (int j = 0; j < 8; j += 4) m[j] = m[j + 1] = m[j + 2] = m[j + 3] = max_nan(m[j], m[j + 2]);
             }
+            Divisor by(0.0f);
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
+                if ((j & (per - 1)) == 0) {
 #pragma unroll
-                for (int o = 16; o; o >>= 1) m[j] = max_nan(m[j], __shfl_xor_sync(~0u, m[j], o));
-                inv[j] = inverse_of(m[j]);
-                const int first = k - lane + 32 * j;
-                if (lane == 0 && first < a.cols && first % a.group == 0) scales[first / a.group] = scale_of(m[j]);
+                    for (int o = 16; o; o >>= 1) m[j] = max_nan(m[j], __shfl_xor_sync(~0u, m[j], o));
+                    const float scale = scale_of(m[j]);
+                    const int first = k - lane + 32 * j;
+                    if (lane == 0 && first < a.cols) scales[first / a.group] = scale;
+                    by = Divisor(scale);
+                }
+                v[j] = by.of(h[c][j]);
             }
         }
-#pragma unroll
-        for (int j = 0; j < 8; ++j) inv[j] *= h[c][j];
-        const uint2 v = codes_of(inv, a.out_dtype);
+        const uint2 b = codes_of(v, a.out_dtype);
         if (WIDE) {
-            if (k < a.cols) *reinterpret_cast<uint2 *>(out + k) = v;
+            if (k < a.cols) *reinterpret_cast<uint2 *>(out + k) = b;
         } else {
 #pragma unroll
             for (int j = 0; j < 8; ++j)
-                if (k + 32 * j < a.cols) out[k + 32 * j] = (uint8_t)((j < 4 ? v.x : v.y) >> (8 * (j & 3)));
+                if (k + 32 * j < a.cols) out[k + 32 * j] = (uint8_t)((j < 4 ? b.x : b.y) >> (8 * (j & 3)));
         }
     }
 }
