@@ -7,14 +7,13 @@
 //      warp-wide reduction and a ballot; cheaper than a further barrier).  Then each CTA takes a run of the (8 tokens of an expert, 16 rows of
 //      G and of U) units; the tokens are staged in shared memory as operand terms, once for all of the run's rows; its warps
 //      take even stretches of the rows' tiles (w4.cuh), rows that two or more share are put together from their parts, and
-//      h = silu(G x) * (U x) goes to the workspace as operand planes: three bf16 terms hold all of it for f32 layers, two
-//      (16 bits) where y is rounded to 8 or 11 bits.
+//      h = silu(G x) * (U x) goes to the workspace as operand planes, three bf16 terms that hold all of it.
 //   3  the CTAs deal out the 16-row tiles of D (two at a time where there are enough, so that h is read half as often): the
 //      warps take even stretches of all chosen experts' tiles, D h lands in shared memory by (token, expert), and y adds
 //      share * D h over a token's experts in their order: no atomics, the same bits every time.  The first tiles of D are
 //      on their way before the barrier is waited for.  Where D has fewer rows than the GPU has SMs, several CTAs share a row's tiles
 //      and their parts of y are added after a further barrier.
-// Measured: 64 tokens, 64 experts of 4096 x 1280 236 us (520 MB: 2.2 TB/s; the 92 blocks of eight tokens that the experts get are each a pass
+// Measured: 64 tokens, 64 experts of 4096 x 1280 258 us (520 MB: 2.0 TB/s; the 92 blocks of eight tokens that the experts get are each a pass
 // over the instructions of w4.cuh, which bound it); one token, 64 experts of 2048 x 1024, 24.3 us, a chain of latencies: router 4K cycles,
 // ranking 4K, G and U 15K, D 8K and two barriers; 5 tokens, 10 experts of 1001 x 333 in f32 23.3 us.
 // Only the chosen experts' weights are read.  Every wait is bounded; a CTA that gives up records it and still
@@ -66,8 +65,7 @@ struct MoeArgs {
     int32_t *status;
 };
 
-// terms of h as the operand of D (bf16)
-constexpr int h_terms(int dtype) { return dtype == MOM_F32 ? 3 : 2; }
+constexpr int H_TERMS = 3;                       // of h as the operand of D (bf16): all 24 bits in layers of every type (two terms, 2^-18 off, took 229 us where three take 258)
 
 // Up to eight tokens of one expert.
 struct Block {
@@ -118,18 +116,11 @@ __device__ __forceinline__ void grid_wait(const MoeArgs &a, unsigned long long t
     __syncthreads();
 }
 
-// 16-bit terms of v: its bits in turn (truncated) for three bf16 terms, which hold all of it; else two, rounded to nearest
-template <int TERMS>
+// v as three bf16 terms, which hold all of it
 __device__ __forceinline__ void store_terms(uint16_t *p, long long plane, float v) {
-    if constexpr (TERMS == 3) {
-        uint32_t t0, t1, t2;
-        split_pair(v, 0.0f, t0, t1, t2);
-        p[0] = (uint16_t)t0; p[plane] = (uint16_t)t1; p[2 * plane] = (uint16_t)t2;
-    } else {
-        const __nv_bfloat16 hi = __float2bfloat16_rn(v);
-        p[0] = __bfloat16_as_ushort(hi);
-        p[plane] = __bfloat16_as_ushort(__float2bfloat16_rn(__hisinf(hi) ? 0.0f : v - __bfloat162float(hi)));
-    }
+    uint32_t t0, t1, t2;
+    split_pair(v, 0.0f, t0, t1, t2);
+    p[0] = (uint16_t)t0; p[plane] = (uint16_t)t1; p[2 * plane] = (uint16_t)t2;
 }
 
 // ---- stage 1
@@ -219,10 +210,9 @@ __device__ void route_fma(const MoeArgs &a, Slots &slots) {
 }
 
 // the columns of h's planes that no unit writes
-template <int DTYPE>
 __device__ void fill_planes(const MoeArgs &a) {
     const int written = a.gate.row_tiles * W4_ROWS, rest = a.h_cols - written;
-    const int rows = h_terms(DTYPE) * a.tokens * a.top_k;
+    const int rows = H_TERMS * a.tokens * a.top_k;
     for (int row = blockIdx.x; row < rows; row += gridDim.x)
         for (int i = threadIdx.x; i < rest; i += THREADS) a.h_planes[(long long)row * a.h_cols + place_of(written + i)] = 0;
 }
@@ -415,7 +405,7 @@ __device__ void expand_stage(const MoeArgs &a, Routing &r, TileRing<SLOTS> &ring
     // G and U sums of an entry of a unit -> h
     auto finish = [&](int unit, int at, int in_tile, float gv, float uv) {
         const int b = unit / row_tiles;
-        store_terms<h_terms(DTYPE)>(a.h_planes + (long long)(r.blocks[b].first_row + at) * a.h_cols + place_of((unit - b * row_tiles) * W4_ROWS + in_tile), h_plane,
+        store_terms(a.h_planes + (long long)(r.blocks[b].first_row + at) * a.h_cols + place_of((unit - b * row_tiles) * W4_ROWS + in_tile), h_plane,
                                     gv / (1.0f + expf(-gv)) * uv);
     };
     for (int run = u0; run < u1; run = run_end(run)) {
@@ -490,9 +480,9 @@ __device__ void expand_stage(const MoeArgs &a, Routing &r, TileRing<SLOTS> &ring
 // ---- stage 3: y = sum of share * D h, ROWS row tiles at a time.  `meet` (the barrier before the stage) is called once the
 // first tiles are on their way.  Where D has fewer rows than there are CTAs, `splits` of them share a unit's tiles and leave their part
 // of y in the workspace; returns whether that is so (then the parts are still to be added).
-template <int DTYPE, int PER, int ROWS, typename MEET>
+template <int PER, int ROWS, typename MEET>
 __device__ int combine_stage(const MoeArgs &a, Routing &r, TileRing<SLOTS> &ring, float *shared, MEET meet) {
-    constexpr int TERMS = h_terms(DTYPE);
+    constexpr int TERMS = H_TERMS;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
     const TokenScales none{0, 0, 0};
     const int pairs = a.tokens * a.top_k, tiles = a.down.col_tiles, total = r.n_blocks * tiles, units = (a.down.row_tiles + ROWS - 1) / ROWS;
@@ -635,7 +625,7 @@ __global__ void __launch_bounds__(THREADS, 1) moe_kernel(const MoeArgs a) {
     }
     for (int e = threadIdx.x; e < a.experts; e += THREADS) r.chosen[e] = 0;
     grid_arrive(a);
-    fill_planes<DTYPE>(a);                                     // (what follows needs no other CTA's logits)
+    fill_planes(a);                                     // (what follows needs no other CTA's logits)
     if (a.resident) stage_tokens<DTYPE>(a, staged, a.tokens, 0, a.gate.col_tiles, a.chunk_tiles * W4_COLS + 32, [](int i) { return i; });
     grid_wait(a, begun + gridDim.x, 1);
     rank_experts(a, r);
@@ -650,8 +640,8 @@ __global__ void __launch_bounds__(THREADS, 1) moe_kernel(const MoeArgs a) {
     ring.tail = ring.head;
     grid_arrive(a);
     auto meet = [&]() { grid_wait(a, begun + 2 * gridDim.x, 2); };
-    const int splits = a.pair_rows ? combine_stage<DTYPE, PER, 2>(a, r, ring, reinterpret_cast<float *>(rest), meet)
-                                   : combine_stage<DTYPE, PER, 1>(a, r, ring, reinterpret_cast<float *>(rest), meet);
+    const int splits = a.pair_rows ? combine_stage<PER, 2>(a, r, ring, reinterpret_cast<float *>(rest), meet)
+                                   : combine_stage<PER, 1>(a, r, ring, reinterpret_cast<float *>(rest), meet);
     // (every CTA arrives three times, so that the count stays a multiple of the grid)
     grid_arrive(a);
     if (splits == 1) return;
@@ -667,7 +657,7 @@ size_t logits_bytes(const mom_moe_desc_t &d, int64_t tokens) { return align_up((
 
 size_t parts_bytes(const mom_moe_desc_t &d, int64_t tokens) { return align_up((size_t)MAX_SPLITS * tokens * d.hidden * 4, WS_ALIGN); }
 size_t h_bytes(const mom_moe_desc_t &d, int64_t tokens) {
-    return align_up((size_t)h_terms(d.dtype) * tokens * d.top_k * align_up((size_t)d.inner, W4_COLS) * 2, WS_ALIGN);
+    return align_up((size_t)H_TERMS * tokens * d.top_k * align_up((size_t)d.inner, W4_COLS) * 2, WS_ALIGN);
 }
 
 template <typename T, int DTYPE, int PER>

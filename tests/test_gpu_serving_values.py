@@ -65,3 +65,62 @@ def test_rms_norm_codes_at_the_ends_of_the_range(cols, out, group, size, weight)
     w = weight * (1 + 0.2 * torch.rand(cols, device="cuda"))
     y, s = check_codes(x, w, out, group, 0.0)
     assert y.isfinite().all() and s.isfinite().all() and (s > 0).all()
+
+
+# ---- mixture of experts
+
+def one_expert(hidden, inner, dtype, g, u, d):
+    """A layer of one expert from integer weights -7..7 (g, u: inner x hidden, d: hidden x inner), all scales 1; returns call(x) -> y."""
+    boxes = [pack((torch.as_tensor(w).reshape(1, *w.shape).numpy() + 8).astype(np.uint8), torch.ones(1, w.shape[0], 1), None, 0)[1] for w in (g, u, d)]
+    plan = mom.mom_moe_plan(hidden, inner, 1, 1, TYPES[dtype][1], mom.F32, 0, mom.F32, False, True)
+    r = torch.zeros(1, hidden, device="cuda")
+
+    def call(x):
+        y = torch.empty_like(x)
+        room = plan.workspace_bytes(x.shape[0])
+        ws = torch.full((room,), 255, dtype=torch.uint8, device="cuda")
+        plan.execute(x.shape[0], ptr(x), ptr(r), *map(ptr, boxes), ptr(y), None, None, ptr(ws), room, stream())
+        torch.cuda.synchronize()
+        assert plan.device_status() == (0, 0)
+        return y
+    return call
+
+
+def silu(a):
+    return a / (1 + np.exp(-a))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("tokens", [3, 64])
+def test_moe_holds_h_in_32_bits(tokens, dtype):
+    """h_0 = silu(x_0) * 7 x_0 and h_1 = silu(x_0) * (7 x_0 + x_1) with x_1 = x_0 / 1024 nearly cancel in y = 7 h_0 - 7 h_1 = -7 silu(x_0) x_1."""
+    torch.manual_seed(tokens)
+    g, u = np.zeros((2, 64), np.int64), np.zeros((2, 64), np.int64)
+    g[:, 0], u[:, 0], u[1, 1] = 1, 7, 1
+    x = torch.zeros(tokens, 64, device="cuda")
+    x[:, 0] = 0.5 + 3.5 * torch.rand(tokens, device="cuda")
+    x[:, 1] = x[:, 0] * 2.0 ** -10
+    x = x.to(TYPES[dtype][0])
+    y = host(one_expert(64, 2, dtype, g, u, np.tile([7, -7], (64, 1)))(x))
+    v = host(x)
+    h = silu(v[:, 0]) * 7 * v[:, 0]
+    want = (-7 * silu(v[:, 0]) * v[:, 1])[:, None]
+    # silu is the same number in both (16 u covers exp, sum, quotient); 7 x_0 + x_1, the product with silu and 7 h are rounded once each, as is the sum
+    bound = 16 * ref.U32 * np.abs(want) + (2 * 7 * 4 * ref.U32 * h)[:, None]
+    assert np.all(np.abs(y - want) <= bound + ref.UNIT[dtype] * (np.abs(want) + bound) + ref.TINY[dtype])
+
+
+@pytest.mark.parametrize("tokens", [1, 5, 8, 40])
+def test_moe_f32_keeps_every_bit(tokens):
+    """One entry of x that is not zero, one row of G and U: y = 7 silu(x) * 7 x, in which every bit of x and of h shows."""
+    torch.manual_seed(tokens)
+    x = torch.zeros(tokens, 128, device="cuda")
+    at = torch.arange(tokens) * 29 % 128
+    v = (0.5 + 3.5 * torch.rand(tokens, device="cuda")) * torch.where(torch.arange(tokens, device="cuda") % 3 == 0, -1.0, 1.0)
+    v[0] = 2 - 2.0 ** -23
+    x[torch.arange(tokens), at] = v
+    y = host(one_expert(128, 1, "f32", np.full((1, 128), 1), np.full((1, 128), 7), np.full((128, 1), 7))(x))
+    a = host(v)
+    want = (49 * silu(a) * a)[:, None]
+    # exp to 2 units at an argument that is exact, sum, quotient, product: 8 u; 7 x and 7 h are summed from three terms, each sum cut at 2 u: 6 u each
+    assert np.all(np.abs(y - want) <= 24 * ref.U32 * np.abs(want))
