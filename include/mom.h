@@ -591,7 +591,8 @@ mom_status_t mom_moe_workspace_bytes(const mom_moe_plan_t *plan, int64_t tokens,
  *   expert_ids    int32, tokens x top_k, largest share first, or NULL;   shares: f32, tokens x top_k, or NULL
  *   workspace     256-byte aligned, borrowed while the enqueued work runs
  * The kernel fills the GPU once and its CTAs meet at barriers (cooperative launch); two executes of one plan must not overlap on the
- * GPU (they share the barrier and the workspace).  A token whose x holds a NaN or an infinity gets NaN entries, the other
+ * GPU (they share the barrier and the workspace), on whichever streams they are.  The first execute of a plan on a device allocates its
+ * device block and clears it on `stream`; it must not be captured into a graph, later ones can.  A token whose x holds a NaN or an infinity gets NaN entries, the other
  * tokens are not affected.  Errors: INVALID_ARG, LIMIT, ALIGNMENT, WORKSPACE_TOO_SMALL, ARCH, ALLOC, CUDA. */
 mom_status_t mom_moe_execute(const mom_moe_plan_t *plan, int64_t tokens, const void *x, int64_t x_stride, const void *router,
                              const void *gate, const void *up, const void *down, void *y, int64_t y_stride,

@@ -755,7 +755,8 @@ mom_status_t mom_moe_execute(const mom_moe_plan_t *plan, int64_t tokens, const v
         plan->block = nullptr;
         plan->device = -1;
         if (cudaMalloc(&plan->block, 64) != cudaSuccess) return MOM_ERR_ALLOC;
-        if (cudaMemset(plan->block, 0, 64) != cudaSuccess) return MOM_ERR_CUDA;
+        // (on the caller's stream: the kernel that follows there must find it cleared, and other streams need not wait for the default one)
+        if (cudaMemsetAsync(plan->block, 0, 64, stream) != cudaSuccess) return MOM_ERR_CUDA;
         plan->device = device;
     }
     MoeArgs a;
@@ -789,7 +790,9 @@ mom_status_t mom_moe_device_status(const mom_moe_plan_t *plan, int32_t *code, in
     int32_t host[2] = {0, 0};
     if (plan->block) {
         if (cudaMemcpy(host, plan->block + 1, sizeof(host), cudaMemcpyDeviceToHost) != cudaSuccess) return MOM_ERR_CUDA;
-        if (host[0] != 0 && cudaMemset(plan->block, 0, 64) != cudaSuccess) return MOM_ERR_CUDA;
+        // (cleared before the call returns: the next execute may come on a stream that does not wait for this one)
+        if (host[0] != 0 && (cudaMemsetAsync(plan->block, 0, 64, cudaStreamLegacy) != cudaSuccess || cudaStreamSynchronize(cudaStreamLegacy) != cudaSuccess))
+            return MOM_ERR_CUDA;
     }
     *code = host[0];
     if (detail) *detail = host[1];

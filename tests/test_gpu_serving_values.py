@@ -124,3 +124,35 @@ def test_moe_f32_keeps_every_bit(tokens):
     want = (49 * silu(a) * a)[:, None]
     # exp to 2 units at an argument that is exact, sum, quotient, product: 8 u; 7 x and 7 h are summed from three terms, each sum cut at 2 u: 6 u each
     assert np.all(np.abs(y - want) <= 24 * ref.U32 * np.abs(want))
+
+
+def test_moe_first_call_on_a_side_stream():
+    """The first execute of a plan, on a stream that does not wait for the default one, while that one is busy: right, and the same bits as later calls."""
+    rng = np.random.default_rng(2)
+    side = torch.cuda.Stream()
+    codes = [weights(rng, 6, *shape, 32, "bf16", False) for shape in ((96, 128), (96, 128), (128, 96))]
+    boxes = [pack(*c, 32)[1] for c in codes]
+    x, r = torch.randn(9, 128, device="cuda").to(torch.bfloat16), torch.randn(6, 128, device="cuda").to(torch.bfloat16) / 11
+    want, ids, _, bound, _, gap = ref.moe(host(x), host(r), *(dense(*c, 32) for c in codes), 2, True)
+    busy, got = torch.randn(8192, 8192, device="cuda"), []
+    big = torch.empty(1 << 28, device="cuda")
+    torch.cuda.synchronize()
+    for _ in range(4):
+        plan = mom.mom_moe_plan(128, 96, 6, 2, mom.BF16, mom.BF16, 32)
+        room = plan.workspace_bytes(9)
+        ws, y = torch.empty(room, dtype=torch.uint8, device="cuda"), torch.empty_like(x)
+        which = torch.empty(9, 2, dtype=torch.int32, device="cuda")
+        torch.cuda.synchronize()
+        for _ in range(8):                                   # some milliseconds of ordinary work on the default stream
+            big.zero_()
+            busy @ busy
+        for _ in range(2):
+            plan.execute(9, ptr(x), ptr(r), *map(ptr, boxes), ptr(y), ptr(which), None, ptr(ws), room, side.cuda_stream)
+            with torch.cuda.stream(side):
+                got.append(y.clone())
+            side.synchronize()
+            assert np.array_equal(which.cpu().numpy(), ids)
+        torch.cuda.synchronize()
+        assert plan.device_status() == (0, 0)
+    assert gap > 1e-5 and all(torch.equal(g, got[0]) for g in got)
+    assert np.all(np.abs(host(got[0]) - want) <= bound + ref.UNIT["bf16"] * (np.abs(want) + bound))
