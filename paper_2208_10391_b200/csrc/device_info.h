@@ -56,6 +56,16 @@ cudaError_t raise_smem_limit_locked(Kernel kernel, int bytes, bool *done) {
 // SM count of the current device (0 on failure).
 int current_sm_count();
 
+// Device memory set to zero, or filled from the host, and there when the call returns.  (cudaMemset, and cudaMemcpy from pageable memory, may return
+// before that and order it on the default stream alone: a kernel on a stream that does not wait for the default one could come first.)
+inline bool cleared(void *p, size_t bytes) {
+    return cudaMemsetAsync(p, 0, bytes, cudaStreamLegacy) == cudaSuccess && cudaStreamSynchronize(cudaStreamLegacy) == cudaSuccess;
+}
+inline bool uploaded(void *p, const void *host, size_t bytes) {
+    return cudaMemcpyAsync(p, host, bytes, cudaMemcpyHostToDevice, cudaStreamLegacy) == cudaSuccess &&
+           cudaStreamSynchronize(cudaStreamLegacy) == cudaSuccess;
+}
+
 // The current device's ordinal and SM count when it is an sm_100 (MOM_OK), else MOM_ERR_ARCH; MOM_ERR_CUDA when it cannot be asked.
 int current_sm100(int *device, int *sm_count);
 

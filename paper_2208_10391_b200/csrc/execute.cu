@@ -6,6 +6,7 @@
 #include <vector>
 
 #include "batched_chain.h"
+#include "device_info.h"
 #include "fused_small.h"
 #include "kernels.h"
 #include "mom_internal.h"
@@ -103,7 +104,7 @@ mom_status_t ensure_device_state(const mom_plan *p, int device) {
     if (!d) return MOM_ERR_ALLOC;
     d->device = device;
     if (cudaMalloc(&d->status, 4 * sizeof(int32_t)) != cudaSuccess) { delete d; return MOM_ERR_ALLOC; }
-    if (cudaMemset(d->status, 0, 4 * sizeof(int32_t)) != cudaSuccess) { cudaFree(d->status); delete d; return MOM_ERR_CUDA; }
+    if (!cleared(d->status, 4 * sizeof(int32_t))) { cudaFree(d->status); delete d; return MOM_ERR_CUDA; }
     p->dev = d;
     return MOM_OK;
 }
@@ -271,7 +272,7 @@ mom_status_t execute_core(const mom_plan *p, const float *const *chain_ptrs, con
             }
             if (!table.empty()) {
                 if (cudaMalloc(&dev->fused_table, table.size() * sizeof(uint2)) != cudaSuccess) return MOM_ERR_ALLOC;
-                if (cudaMemcpy(dev->fused_table, table.data(), table.size() * sizeof(uint2), cudaMemcpyHostToDevice) != cudaSuccess) return MOM_ERR_CUDA;
+                if (!uploaded(dev->fused_table, table.data(), table.size() * sizeof(uint2))) return MOM_ERR_CUDA;
             }
         }
         fp.copy_table = dev->fused_table;
@@ -958,7 +959,7 @@ mom_status_t mom_plan_device_status(const mom_plan_t *plan, int32_t *code, int32
     int32_t host[4] = {0, 0, 0, 0};
     if (plan->dev && plan->dev->status) {
         if (cudaMemcpy(host, plan->dev->status, sizeof(host), cudaMemcpyDeviceToHost) != cudaSuccess) return MOM_ERR_CUDA;
-        if (host[0] != 0 && cudaMemset(plan->dev->status, 0, sizeof(host)) != cudaSuccess) return MOM_ERR_CUDA;
+        if (host[0] != 0 && !mom::cleared(plan->dev->status, sizeof(host))) return MOM_ERR_CUDA;
     }
     *code = host[0];
     if (detail) *detail = host[1];

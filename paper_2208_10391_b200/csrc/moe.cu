@@ -785,14 +785,13 @@ mom_status_t mom_moe_execute(const mom_moe_plan_t *plan, int64_t tokens, const v
 }
 
 mom_status_t mom_moe_device_status(const mom_moe_plan_t *plan, int32_t *code, int32_t *detail) {
+    using namespace mom;
     if (!plan || !code) return MOM_ERR_INVALID_ARG;
     std::lock_guard<std::mutex> lock(plan->mutex);
     int32_t host[2] = {0, 0};
     if (plan->block) {
         if (cudaMemcpy(host, plan->block + 1, sizeof(host), cudaMemcpyDeviceToHost) != cudaSuccess) return MOM_ERR_CUDA;
-        // (cleared before the call returns: the next execute may come on a stream that does not wait for this one)
-        if (host[0] != 0 && (cudaMemsetAsync(plan->block, 0, 64, cudaStreamLegacy) != cudaSuccess || cudaStreamSynchronize(cudaStreamLegacy) != cudaSuccess))
-            return MOM_ERR_CUDA;
+        if (host[0] != 0 && !cleared(plan->block, 64)) return MOM_ERR_CUDA;
     }
     *code = host[0];
     if (detail) *detail = host[1];

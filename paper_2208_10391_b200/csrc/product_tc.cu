@@ -944,7 +944,7 @@ mom_status_t tc_prepare(const mom_plan &p, TcPlanState &s) {
     int4 *cur = static_cast<int4 *>(s.block);
     for (int i = 0; i < ns; ++i) {
         if (tables[i].empty()) continue;
-        if (cudaMemcpy(cur, tables[i].data(), tables[i].size() * sizeof(int4), cudaMemcpyHostToDevice) != cudaSuccess) {
+        if (!uploaded(cur, tables[i].data(), tables[i].size() * sizeof(int4))) {
             cudaFree(s.block);
             s.block = nullptr;
             return MOM_ERR_CUDA;
@@ -955,7 +955,7 @@ mom_status_t tc_prepare(const mom_plan &p, TcPlanState &s) {
         for (int q = 0; q < 2; ++q) {
             const std::vector<int4> &pt = part_tables[q][i];
             if (pt.empty()) continue;
-            if (cudaMemcpy(cur, pt.data(), pt.size() * sizeof(int4), cudaMemcpyHostToDevice) != cudaSuccess) {
+            if (!uploaded(cur, pt.data(), pt.size() * sizeof(int4))) {
                 cudaFree(s.block);
                 s.block = nullptr;
                 return MOM_ERR_CUDA;
