@@ -245,8 +245,11 @@ __global__ void __launch_bounds__(1024) rms_norm_kernel(NormArgs a) {
                 load_batch(a.weight, a.weight_dtype, [&](int j) { return min(k + 32 * j, a.cols - 1); }, w);
             }
         }
+        // (8 bits: entries beyond the last column stay 0; an infinite factor or weight would make a NaN of them, which the scale would take up)
+        const float f = CODES && WIDE && k >= a.cols ? 0.0f : factor;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) h[c][j] = h[c][j] * factor * w[j];
+        for (int j = 0; j < 8; ++j)
+            if (!CODES || WIDE || k + 32 * j < a.cols) h[c][j] = h[c][j] * f * w[j];
     }
 
     if (!CODES) {

@@ -67,6 +67,24 @@ def test_rms_norm_codes_at_the_ends_of_the_range(cols, out, group, size, weight)
     assert y.isfinite().all() and s.isfinite().all() and (s > 0).all()
 
 
+@pytest.mark.parametrize("cols", [33, 40, 95, 200, 1001])
+@pytest.mark.parametrize("out,group", [("e4m3", 0), ("e4m3", 32), ("int8", 128)])
+def test_rms_norm_infinite_weight_in_the_last_column(cols, out, group):
+    """The last group's scale is infinite, as the formula says, and not NaN; other groups have theirs."""
+    torch.manual_seed(cols)
+    x, w = torch.randn(3, cols, device="cuda"), 1 + torch.rand(cols, device="cuda")
+    w[-1] = float("inf")
+    y, s = check_codes(x, w, out, group)
+    assert y[:, -1].isinf().all() and s[:, -1].isinf().all() and s[:, :-1].isfinite().all()
+
+
+@pytest.mark.parametrize("cols", [33, 40, 200, 1001])
+def test_rms_norm_squares_that_vanish(cols):
+    """eps = 0 and entries whose squares are below f32: the factor is infinite and so is y; no column beyond the last makes a NaN of the scale."""
+    y, s = check_codes(1e-25 * (1 + torch.rand(3, cols, device="cuda")), torch.ones(cols, device="cuda"), "e4m3", 128, 0.0)
+    assert y.isinf().all() and s.isinf().all()
+
+
 # ---- mixture of experts
 
 def one_expert(hidden, inner, dtype, g, u, d):
