@@ -3,7 +3,7 @@
 // One CTA per row, or one warp where there are many short rows.  A thread keeps its entries of h = x + residual in registers as
 // f32 (8 per chunk, up to four chunks), so that x and the residual are read once and everything that follows (sum of squares, the
 // row's factor, the groups' largest entries, the codes) happens on chip: the kernel moves what it cannot do without and is bound
-// by HBM for many rows, by one chain of load - reduction - store latencies for few.  Measured: 8192 x 8192 bf16 to e4m3 87 us
+// by HBM for many rows, by one chain of load - reduction - store latencies for few.  Measured: 8192 x 8192 bf16 to e4m3 88 us
 // (5.4 TB/s of the 6.5 that a copy reaches), 4096 x 4096 in f32 42.1 us (6.4 TB/s), 1 x 4096 3.5 us (a launch of an empty kernel
 // takes as long).
 //   wide    a thread's 8 entries are consecutive: one 16-byte load per 16-bit tensor; a group of 32 / 64 / 128 columns
@@ -11,7 +11,6 @@
 //   narrow  (rows that are not 16-byte addressable or of a length that is not a multiple of 8): entry j of a lane is
 //           column 32 j + lane of its warp's 256, so that a warp's loads and stores are contiguous; a group is one, two or
 //           four of these.
-#include <algorithm>
 #include <cmath>
 #include <type_traits>
 
@@ -140,30 +139,42 @@ __device__ __forceinline__ uint2 codes_of(const float (&v)[8], int dtype) {
     return make_uint2(__byte_perm(b[0], b[1], 0x5410), __byte_perm(b[2], b[3], 0x5410));
 }
 
-// Over the row's warps (those with no entries hand in the neutral 0); every thread gets the result.
-template <bool MAX, bool WARP>
-__device__ __forceinline__ float row_reduce(float v, float *slots) {
+// The row's sum from each lane's sum, or, TWO, from its sums of two warps' worth of columns; every thread gets the result.
+template <bool TWO, bool WARP>
+__device__ __forceinline__ float row_sum(float v, float second, float *slots) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = (TWO ? 2 : 1) * (blockDim.x >> 5);
+    if (TWO) v = (lane & 16 ? second : v) + __shfl_xor_sync(~0u, lane & 16 ? v : second, 16);       // half of the lanes go on with each
+    else v += __shfl_xor_sync(~0u, v, 16);
 #pragma unroll
-    for (int o = 16; o; o >>= 1) {
-        const float u = __shfl_xor_sync(~0u, v, o);
-        v = MAX ? max_nan(v, u) : v + u;
-    }
+    for (int o = 8; o; o >>= 1) v += __shfl_xor_sync(~0u, v, o);
+    if (WARP || warps == 1) return v;
+    if ((lane & (TWO ? 15 : 31)) == 0) slots[TWO ? 2 * warp + (lane >> 4) : warp] = v;
+    __syncthreads();
+    v = lane < warps ? slots[lane] : 0.0f;
+    if (TWO) v += lane + 32 < warps ? slots[lane + 32] : 0.0f;
+#pragma unroll
+    for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(~0u, v, o);
+    return v;
+}
+
+// The row's largest entry; warps with no entries hand in 0, every thread gets the result.
+template <bool WARP>
+__device__ __forceinline__ float row_max(float v, float *slots) {
+#pragma unroll
+    for (int o = 16; o; o >>= 1) v = max_nan(v, __shfl_xor_sync(~0u, v, o));
     const int warps = blockDim.x >> 5;
     if (WARP || warps == 1) return v;
     if ((threadIdx.x & 31) == 0) slots[threadIdx.x >> 5] = v;
     __syncthreads();
     v = (threadIdx.x & 31) < warps ? slots[threadIdx.x & 31] : 0.0f;
 #pragma unroll
-    for (int o = 16; o; o >>= 1) {
-        const float u = __shfl_xor_sync(~0u, v, o);
-        v = MAX ? max_nan(v, u) : v + u;
-    }
+    for (int o = 16; o; o >>= 1) v = max_nan(v, __shfl_xor_sync(~0u, v, o));
     return v;
 }
 
 template <typename T, bool WIDE, bool CODES, int CHUNKS, bool WARP>          // WARP: a warp per row
 __global__ void __launch_bounds__(1024) rms_norm_kernel(NormArgs a) {
-    __shared__ float slots[2][32];
+    __shared__ float sums[64], largest[32];
     const int lane = threadIdx.x & 31, warp = WARP ? 0 : threadIdx.x >> 5;
     const long long row = WARP ? (long long)blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5) : blockIdx.x;
     if (WARP && row >= a.rows) return;                           // (a whole warp, and then no barrier follows)
@@ -171,15 +182,17 @@ __global__ void __launch_bounds__(1024) rms_norm_kernel(NormArgs a) {
     const T *res = a.residual ? static_cast<const T *>(a.residual) + row * a.residual_stride : nullptr;
     T *res_out = a.residual_out ? static_cast<T *>(a.residual_out) + row * a.residual_stride : nullptr;
 
-    // column of entry j of chunk c
+    // Column of entry j of chunk c: a warp has 256 neighbouring ones of a chunk.  Four chunks: those that two neighbouring warps have with two
+    // chunks, so that every sum has the same bits.
+    const int half = (a.cols + 511) / 512;
     auto column = [&](int c, int j) {
-        if (WARP) return c * 256 + (WIDE ? lane * 8 + j : j * 32 + lane);
-        return c * (int)blockDim.x * 8 + (WIDE ? (int)threadIdx.x * 8 + j : warp * 256 + j * 32 + lane);
+        const int k = WIDE ? lane * 8 + j : j * 32 + lane;
+        if (CHUNKS == 4) return 2 * warp * 256 + k + (c & 1) * half * 256 + (c >> 1) * (2 * warp + 1 < half ? 256 : a.cols);
+        return (WARP ? c : c * (int)(blockDim.x >> 5) + warp) * 256 + k;
     };
 
     grid_dependency_wait();                              // nothing has been read yet
-    float h[CHUNKS][8];
-    float sum = 0.0f;
+    float h[CHUNKS][8], sum = 0.0f, second = 0.0f;
     if (WIDE) {                                          // every load under way before the first is used
         Eight<T> v[CHUNKS], r[CHUNKS];
 #pragma unroll
@@ -221,10 +234,11 @@ __global__ void __launch_bounds__(1024) rms_norm_kernel(NormArgs a) {
                     if (k + 32 * j < a.cols) res_out[k + 32 * j] = from_float<T>(h[c][j]);
             }
         }
+        float &s = c < 2 ? sum : second;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) sum = fmaf(h[c][j], h[c][j], sum);
+        for (int j = 0; j < 8; ++j) s = fmaf(h[c][j], h[c][j], s);
     }
-    const float factor = 1.0f / sqrtf(row_reduce<false, WARP>(sum, slots[0]) / (float)a.cols + a.eps);
+    const float factor = 1.0f / sqrtf(row_sum<(CHUNKS > 2), WARP>(sum, second, sums) / (float)a.cols + a.eps);
 
     allow_dependents();
     // y = h * factor * weight
@@ -278,13 +292,12 @@ __global__ void __launch_bounds__(1024) rms_norm_kernel(NormArgs a) {
     uint8_t *out = static_cast<uint8_t *>(a.out) + row * a.out_stride;
     float row_scale = 0.0f;
     if (a.group == 0) {
-        float row_max = 0.0f;
+        float m = 0.0f;
 #pragma unroll
         for (int c = 0; c < CHUNKS; ++c)
 #pragma unroll
-            for (int j = 0; j < 8; ++j) row_max = max_nan(row_max, fabsf(h[c][j]));
-        row_max = row_reduce<true, WARP>(row_max, slots[1]);
-        row_scale = scale_of(row_max);
+            for (int j = 0; j < 8; ++j) m = max_nan(m, fabsf(h[c][j]));
+        row_scale = scale_of(row_max<WARP>(m, largest));
         if ((WARP ? lane : threadIdx.x) == 0) scales[0] = row_scale;
     }
     const Divisor by_row(row_scale);
@@ -347,17 +360,23 @@ template <typename T, bool WIDE>
 cudaError_t launch(NormArgs a, int64_t rows, int sm_count, cudaStream_t stream) {
     // Few rows: a thread holds 8 entries (one chain of latencies, as many threads as it takes).  Many rows of up to 512 columns: a warp
     // each, so that CTAs are not the cost (8000 x 320 in bf16 10.1 -> 4.8 us; from 1024 columns on a CTA per row is as good or better).
-    // Many longer rows, us with 1 / 2 / 4 chunks of 8 entries a thread: f32 or narrow one chunk (809 x 6728 in f32 17.7 / 18.8 / 22.2,
-    // 2048 x 4099 19.6 / 21.6 / 48), 16 bits two (1859 x 7176 22.6 / 19.9 / 20.9, 2000 x 12288 - / 33.1 / 35.2), four where that fills
-    // eight warps (8192 x 8192 107 / 90 / 86).
+    // Many longer rows: f32 or narrow one chunk (us with 1 / 2 / 4 chunks: 809 x 6728 in f32 17.7 / 18.8 / 22.2, 2048 x 4099 19.6 / 21.6 / 48).
+    // 16 bits two, and four with 8-bit outputs (64 registers a thread, 32 warps on an SM, where two chunks take 40 and leave 48) if an SM then holds
+    // at least a quarter more rows at once.  Rows of 32 M entries in all, us with 2 / 4 chunks: to e4m3, a scale per 128, 2304 columns
+    // 49.1 / 55.0, 3328 50.2 / 51.9, 4096 47.0 / 46.5, 5120 50.1 / 48.2, 6656 51.9 / 52.2, 7424 50.9 / 50.5, 8192 49.1 / 48.1, 9216 55.3 / 51.8,
+    // 10496 54.2 / 60.8, 12288 51.6 / 55.3, 12544 75.0 / 55.9, 16384 66.6 / 51.1; a scale per row 4096 43.0 / 41.2, 7424 48.0 / 44.6,
+    // 10496 50.7 / 52.6, 16384 62.1 / 45.6.  f16 to f16 2304 41.7 / 43.4, 4096 42.3 / 44.2, 8192 43.1 / 44.8, 12288 44.3 / 44.8, 16384 44.0 / 45.5.
     const int pieces = (a.cols + 255) / 256;                          // warps' worth of columns
+    const bool codes = !is_float_type(a.out_dtype);
     int chunks = pieces <= 32 ? 1 : pieces <= 64 ? 2 : 4;
-    if (rows > 2 * sm_count && WIDE && sizeof(T) == 2 && pieces > 8) chunks = std::max(chunks, pieces == 31 || pieces == 32 ? 4 : 2);
+    if (rows > 2 * sm_count && WIDE && sizeof(T) == 2 && pieces > 8 && pieces <= 64) {
+        const int by_two = 48 / ((pieces + 1) / 2), by_four = 32 / ((pieces + 3) / 4);
+        chunks = codes && 4 * by_four >= 5 * by_two ? 4 : 2;
+    }
     const bool warp_rows = rows > 8 * sm_count && pieces <= 2;
     a.rows = (int)rows;
     const int threads = warp_rows ? 256 : 32 * ((pieces + chunks - 1) / chunks);
     const dim3 grid((unsigned)(warp_rows ? (rows + 7) / 8 : rows));
-    const bool codes = !is_float_type(a.out_dtype);
     void (*kernel)(NormArgs);
     if (warp_rows)
         kernel = pieces == 1 ? (codes ? rms_norm_kernel<T, WIDE, true, 1, true> : rms_norm_kernel<T, WIDE, false, 1, true>)

@@ -174,3 +174,11 @@ def test_moe_first_call_on_a_side_stream():
         assert plan.device_status() == (0, 0)
     assert gap > 1e-5 and all(torch.equal(g, got[0]) for g in got)
     assert np.all(np.abs(host(got[0]) - want) <= bound + ref.UNIT["bf16"] * (np.abs(want) + bound))
+
+
+@pytest.mark.parametrize("cols", [2304, 4099, 5120, 7424, 8192, 8448, 10496, 12544, 16384])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_rms_norm_widths_of_many_rows(cols, dtype):
+    """However a launch cuts its rows (by width and output), the codes come from the y of the float output."""
+    torch.manual_seed(cols)
+    check_codes(torch.randn(320, cols, device="cuda").to(TYPES[dtype][0]), 1 + 0.3 * torch.randn(cols, device="cuda"), "e4m3", 128)
