@@ -182,3 +182,85 @@ def test_rms_norm_widths_of_many_rows(cols, dtype):
     """However a launch cuts its rows (by width and output), the codes come from the y of the float output."""
     torch.manual_seed(cols)
     check_codes(torch.randn(320, cols, device="cuda").to(TYPES[dtype][0]), 1 + 0.3 * torch.randn(cols, device="cuda"), "e4m3", 128)
+
+
+# ---- product with 4-bit weights, on both sides of the choice of kernel (more than eight tokens: tcgen05)
+
+@pytest.mark.parametrize("tokens", [1, 2, 5, 8, 9, 20])
+@pytest.mark.parametrize("cols", [128, 1003])
+@pytest.mark.parametrize("zeros", [False, True])
+def test_w4_product_f32_keeps_every_bit(tokens, cols, zeros):
+    """One entry a token that is not zero, all scales 1: the three terms of an entry times a code are summed, each sum cut at 2^-23 at most."""
+    torch.manual_seed(tokens + cols)
+    codes, s, z = weights(np.random.default_rng(tokens), 1, 48, cols, 32, "f32", zeros)
+    s = torch.ones_like(s)
+    d, box = pack(codes, s, z, 32)
+    x = torch.zeros(tokens, cols, device="cuda")
+    v = (0.5 + 3.5 * torch.rand(tokens, device="cuda")) * 2.0 ** torch.randint(-60, 60, (tokens,), device="cuda")
+    v[0] = -(2 - 2.0 ** -23)
+    x[torch.arange(tokens), torch.arange(tokens) * 37 % cols] = v
+    y = torch.empty(tokens, 48, device="cuda")
+    mom.mom_w4_product(mom.mom_w4_product_desc(d, tokens, mom.F32, mom.F32), ptr(box), ptr(x), None, None, ptr(y), stream())
+    torch.cuda.synchronize()
+    want = host(x) @ dense(codes, s, z, 32)[0].T
+    assert np.all(np.abs(host(y) - want) <= 2.0 ** -22 * np.abs(want))
+
+
+@pytest.mark.parametrize("tokens", [1, 3, 5, 8, 9, 11, 33])
+@pytest.mark.parametrize("kind", ["f32", "bf16", "f16"])
+def test_w4_product_special_values(tokens, kind):
+    """NaN and infinities stay in their token, also in the last one, whose row stands in for tokens that are not there; the others keep their bits."""
+    torch.manual_seed(tokens)
+    codes, s, z = weights(np.random.default_rng(4), 1, 40, 96, 32, "f32", False)
+    codes[codes == 8] = 9                               # no weight is zero
+    d, box = pack(codes, s, z, 32)
+    w = torch.from_numpy(dense(codes, s, z, 32)[0]).cuda()
+    clean = torch.randn(tokens, 96, device="cuda").to(TYPES[kind][0])
+    p = mom.mom_w4_product_desc(d, tokens, TYPES[kind][1], mom.F32)
+
+    def product(x):
+        y = torch.full((tokens, 40), 5.0, device="cuda")
+        mom.mom_w4_product(p, ptr(box), ptr(x), None, None, ptr(y), stream())
+        torch.cuda.synchronize()
+        return y
+    y0 = product(clean)
+    for at in sorted({0, tokens // 2, tokens - 1}):
+        for value, col in ((float("nan"), 3), (float("inf"), 70), (float("-inf"), 1)):
+            x = clean.clone()
+            x[at, col] = value
+            y = product(x)
+            others = [i for i in range(tokens) if i != at]
+            assert torch.equal(y[others], y0[others])
+            if value != value:
+                assert y[at].isnan().all()
+            else:
+                assert torch.equal(y[at], torch.sign(w[:, col]).float() * value)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("tokens", [2, 10])
+def test_moe_special_tokens_keep_the_others_bits(tokens, dtype):
+    """A router of zeros sends every token to the first experts, whatever it holds, so that nothing is dealt out otherwise: the other tokens have the same bits."""
+    torch.manual_seed(tokens)
+    rng = np.random.default_rng(tokens)
+    boxes = [pack(*weights(rng, 5, *shape, 32, "bf16", False), 32)[1] for shape in ((64, 128), (64, 128), (128, 64))]
+    t, kind = TYPES[dtype]
+    r = torch.zeros(5, 128, device="cuda", dtype=t)
+    plan = mom.mom_moe_plan(128, 64, 5, 2, kind, kind, 32)
+    room = plan.workspace_bytes(tokens)
+    ws = torch.empty(room, dtype=torch.uint8, device="cuda")
+
+    def layer(x):
+        y, ids = torch.empty_like(x), torch.empty(tokens, 2, dtype=torch.int32, device="cuda")
+        plan.execute(tokens, ptr(x), ptr(r), *map(ptr, boxes), ptr(y), ptr(ids), None, ptr(ws), room, stream())
+        torch.cuda.synchronize()
+        assert plan.device_status() == (0, 0) and ids.cpu().tolist() == [[0, 1]] * tokens
+        return y
+    x = torch.randn(tokens, 128, device="cuda").to(t)
+    y0 = layer(x)
+    for at, value in ((tokens - 1, float("nan")), (0, float("inf")), (tokens // 2, float("-inf"))):
+        special = x.clone()
+        special[at, 5] = value
+        y = layer(special)
+        others = [i for i in range(tokens) if i != at]
+        assert torch.equal(y[others], y0[others]) and y[at].isnan().all()
