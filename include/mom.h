@@ -598,8 +598,13 @@ mom_status_t mom_moe_execute(const mom_moe_plan_t *plan, int64_t tokens, const v
                              const void *gate, const void *up, const void *down, void *y, int64_t y_stride,
                              int32_t *expert_ids, float *shares, void *workspace, size_t workspace_bytes, mom_stream_t stream);
 
-/* As mom_plan_device_status, for the barriers of mom_moe_execute. */
+/* As mom_plan_device_status, for the barriers of mom_moe_execute (detail: which barrier).  Where a wait gave up, which takes a defect of the GPU or of this
+ * library, the y of that execute is NaN in all that may be wrong, and expert_ids and shares are not defined; later executes are not affected. */
 mom_status_t mom_moe_device_status(const mom_moe_plan_t *plan, int32_t *code, int32_t *detail);
+
+/* Self-test of that route: the plan's next execute waits at each of its barriers for one arrival that never comes and gives up after `limit_ms`
+ * (0 < limit_ms <= 1000).  Errors: INVALID_ARG. */
+mom_status_t mom_moe_probe_wait_timeout(const mom_moe_plan_t *plan, double limit_ms);
 
 /* Sustained-rate probes used as roofline denominators.  Each runs an instruction-issue loop on every
  * SM for about `milliseconds` and returns the achieved rate; no global memory traffic besides a

@@ -142,6 +142,7 @@ _sigs = {
     "mom_moe_workspace_bytes": [_P, ctypes.c_int64, ctypes.POINTER(ctypes.c_size_t)],
     "mom_moe_execute": [_P, ctypes.c_int64, _P, ctypes.c_int64, _P, _P, _P, _P, _P, ctypes.c_int64, _P, _P, _P, ctypes.c_size_t, _P],
     "mom_moe_device_status": [_P, ctypes.POINTER(ctypes.c_int32), ctypes.POINTER(ctypes.c_int32)],
+    "mom_moe_probe_wait_timeout": [_P, ctypes.c_double],
     "mom_probe_tf32_tflops": [ctypes.c_double, _P, _P, ctypes.POINTER(ctypes.c_double)],
     "mom_probe_ffma_tflops": [ctypes.c_double, _P, _P, ctypes.POINTER(ctypes.c_double)],
 }
@@ -596,6 +597,10 @@ class MoePlan:
         code, detail = ctypes.c_int32(), ctypes.c_int32()
         _check(_lib.mom_moe_device_status(self._h, code, detail), "mom_moe_device_status")
         return code.value, detail.value
+
+    def probe_wait_timeout(self, limit_ms: float) -> None:
+        """The next execute's waits run out after `limit_ms` (self-test of the bounded waits)."""
+        _check(_lib.mom_moe_probe_wait_timeout(self._h, limit_ms), "mom_moe_probe_wait_timeout")
 
 
 def mom_moe_plan(hidden: int, inner: int, experts: int, top_k: int, dtype: int, router_dtype: int, group: int = 128, scale_dtype: int = BF16,

@@ -16,8 +16,8 @@
 // Measured: 64 tokens, 64 experts of 4096 x 1280 258 us (520 MB: 2.0 TB/s; the 92 blocks of eight tokens that the experts get are each a pass
 // over the instructions of w4.cuh, which bound it); one token, 64 experts of 2048 x 1024, 24.3 us, a chain of latencies: router 4K cycles,
 // ranking 4K, G and U 15K, D 8K and two barriers; 5 tokens, 10 experts of 1001 x 333 in f32 23.3 us.
-// Only the chosen experts' weights are read.  Every wait is bounded; a CTA that gives up records it and still
-// arrives at the next barrier, so that nobody waits for it.
+// Only the chosen experts' weights are read.  Every wait is bounded; a CTA that gives up records it and still arrives at the next barrier, so
+// that nobody waits for it; it writes NaN for its part of y, and so do all that meet it at a later barrier.
 #include <algorithm>
 #include <cmath>
 
@@ -32,7 +32,8 @@ struct mom_moe_plan {
     mom_w4_desc_t gate, down;                // U has G's
     mutable std::mutex mutex;
     mutable int device = -1;
-    mutable unsigned long long *block = nullptr;   // [0] barrier arrivals, then the status word
+    mutable unsigned long long *block = nullptr;   // [0] barrier arrivals, then the status words
+    mutable unsigned long long probe_ns = 0;       // self-test: the next execute's waits run out after so long
 };
 
 namespace mom {
@@ -63,6 +64,8 @@ struct MoeArgs {
     float *shares;
     unsigned long long *arrivals;
     int32_t *status;
+    unsigned long long limit_ns;
+    int missing;                   // self-test: arrivals that are waited for and never come
 };
 
 constexpr int H_TERMS = 3;                       // of h as the operand of D (bf16): all 24 bits in layers of every type (two terms, 2^-18 off, took 229 us where three take 258)
@@ -78,7 +81,7 @@ struct alignas(16) Routing {
     unsigned char token[MAX_PAIRS];            // of a row of h
     short ids[MAX_T][MAX_K], row[MAX_T][MAX_K];    // a token's experts, its rows of h
     float shares[MAX_T][MAX_K];
-    int n_blocks;
+    int n_blocks, fine;                        // fine: no wait of this launch is known to have given up
 };
 // Shared memory: Routing, the warps' rings, then by stage
 //   1  Slots                                             2  Part, sums over chunks (where x is staged in chunks), x
@@ -91,27 +94,35 @@ struct Part { float v[WARPS][2][2][TOKENS][LD]; };              // a stretch's f
 struct Sums { float v[BATCH][2][TOKENS][LD]; };
 template <int ROWS> struct DownPart { float v[WARPS][2][ROWS][TOKENS][LD]; };
 
-// All CTAs of the grid meet.  The count only grows and every CTA of every launch arrives at every barrier, so that it is a
-// multiple of the grid between launches: `target` counts on from the multiple that was read when the kernel began.
-__device__ __forceinline__ void grid_arrive(const MoeArgs &a) {
+// All CTAs of the grid meet.  The count (the lower 48 bits) only grows and every CTA of every launch arrives at every barrier, so that it is a
+// multiple of the grid between launches: targets count on from the multiple that was read when the kernel began.  A CTA whose wait gave
+// up adds to the upper bits with all its later arrivals, so that everyone who meets it there learns of it without a further load.
+constexpr unsigned long long GAVE_UP = 1ull << 48, COUNT = GAVE_UP - 1;
+__device__ __forceinline__ void grid_arrive(const MoeArgs &a, const Routing &r) {
     __syncthreads();
-    if (threadIdx.x == 0) asm volatile("fence.acq_rel.gpu;\n\tred.relaxed.gpu.global.add.u64 [%0], 1;" ::"l"(a.arrivals) : "memory");
+    if (threadIdx.x == 0)
+        asm volatile("fence.acq_rel.gpu;\n\tred.relaxed.gpu.global.add.u64 [%0], %1;" ::"l"(a.arrivals), "l"(r.fine ? 1ull : GAVE_UP + 1) : "memory");
 }
-__device__ __forceinline__ void grid_wait(const MoeArgs &a, unsigned long long target, int detail) {
+// `begun`: what the count was when the launch began.  Clears r.fine once a wait of the launch has given up: one of this CTA, or of another
+// before it arrived here.
+__device__ __forceinline__ void grid_wait(const MoeArgs &a, Routing &r, unsigned long long begun, int barrier) {
     if (threadIdx.x == 0) {
+        const unsigned long long target = (begun & COUNT) + (unsigned)barrier * gridDim.x + a.missing;
         unsigned long long start = 0, seen;
         for (unsigned i = 0;; ++i) {
             asm volatile("ld.acquire.gpu.global.u64 %0, [%1];" : "=l"(seen) : "l"(a.arrivals) : "memory");
-            if (seen >= target) break;
+            if ((seen & COUNT) >= target) break;
             if ((i & 63) == 63) {
                 const unsigned long long now = global_ns();
                 if (start == 0) start = now;
-                else if (now - start > WAIT_LIMIT_NS) {
-                    if (atomicCAS(a.status, 0, (int)MOM_ERR_DEVICE_TIMEOUT) == 0) a.status[1] = detail;
+                else if (now - start > a.limit_ns) {
+                    if (atomicCAS(a.status, 0, (int)MOM_ERR_DEVICE_TIMEOUT) == 0) a.status[1] = barrier;
+                    r.fine = 0;
                     break;
                 }
             }
         }
+        if ((seen ^ begun) >= GAVE_UP) r.fine = 0;
     }
     __syncthreads();
 }
@@ -593,6 +604,7 @@ __device__ int combine_stage(const MoeArgs &a, Routing &r, TileRing<SLOTS> &ring
             float v = 0.0f;
             for (int j = 0; j < a.top_k; ++j) v = fmaf(r.shares[token][j], by_row[(m * pairs + r.row[token][j]) * LD + in_tile], v);
             if (row >= a.hidden) continue;
+            if (!r.fine) v = __int_as_float(0x7fffffff);
             if (splits > 1) a.parts[((long long)split * a.tokens + token) * a.hidden + row] = v;
             else store_from_float(a.y, token * a.y_stride + row, a.dtype, v);
         }
@@ -615,7 +627,8 @@ __global__ void __launch_bounds__(THREADS, 1) moe_kernel(const MoeArgs a) {
     unsigned long long begun = 0;                              // what earlier launches left the count at
     if (threadIdx.x == 0) {
         asm volatile("ld.relaxed.gpu.global.u64 %0, [%1];" : "=l"(begun) : "l"(a.arrivals) : "memory");
-        begun -= begun % gridDim.x;
+        begun -= (begun & COUNT) % gridDim.x;
+        r.fine = 1;
     }
     if constexpr (DTYPE == MOM_F32) {
         route_fma<T, float>(a, *reinterpret_cast<Slots *>(rest));
@@ -624,10 +637,10 @@ __global__ void __launch_bounds__(THREADS, 1) moe_kernel(const MoeArgs a) {
         else route_mma<DTYPE>(a, *reinterpret_cast<Slots *>(rest));
     }
     for (int e = threadIdx.x; e < a.experts; e += THREADS) r.chosen[e] = 0;
-    grid_arrive(a);
+    grid_arrive(a, r);
     fill_planes(a);                                     // (what follows needs no other CTA's logits)
     if (a.resident) stage_tokens<DTYPE>(a, staged, a.tokens, 0, a.gate.col_tiles, a.chunk_tiles * W4_COLS + 32, [](int i) { return i; });
-    grid_wait(a, begun + gridDim.x, 1);
+    grid_wait(a, r, begun, 1);                                    // (given up: the next barrier says so to all)
     rank_experts(a, r);
 
     TileRing<SLOTS> ring((uint32_t)__cvta_generic_to_shared(rings + warp * ring_bytes), a.gate);
@@ -638,17 +651,18 @@ __global__ void __launch_bounds__(THREADS, 1) moe_kernel(const MoeArgs a) {
     __syncthreads();
     asm volatile("cp.async.wait_all;" ::: "memory");
     ring.tail = ring.head;
-    grid_arrive(a);
-    auto meet = [&]() { grid_wait(a, begun + 2 * gridDim.x, 2); };
+    grid_arrive(a, r);
+    auto meet = [&]() { grid_wait(a, r, begun, 2); };
     const int splits = a.pair_rows ? combine_stage<PER, 2>(a, r, ring, reinterpret_cast<float *>(rest), meet)
                                    : combine_stage<PER, 1>(a, r, ring, reinterpret_cast<float *>(rest), meet);
     // (every CTA arrives three times, so that the count stays a multiple of the grid)
-    grid_arrive(a);
+    grid_arrive(a, r);
     if (splits == 1) return;
-    grid_wait(a, begun + 3 * gridDim.x, 3);
+    grid_wait(a, r, begun, 3);
     for (long long i = (long long)blockIdx.x * THREADS + threadIdx.x; i < (long long)a.tokens * a.hidden; i += (long long)gridDim.x * THREADS) {
         float v = 0.0f;
         for (int p = 0; p < splits; ++p) v += a.parts[(long long)p * a.tokens * a.hidden + i];
+        if (!r.fine) v = __int_as_float(0x7fffffff);
         store_from_float(a.y, i / a.hidden * a.y_stride + i % a.hidden, a.dtype, v);
     }
 }
@@ -777,6 +791,9 @@ mom_status_t mom_moe_execute(const mom_moe_plan_t *plan, int64_t tokens, const v
     a.ids = expert_ids; a.shares = shares;
     a.arrivals = plan->block;
     a.status = reinterpret_cast<int32_t *>(plan->block + 1);
+    a.missing = plan->probe_ns != 0;
+    a.limit_ns = plan->probe_ns ? plan->probe_ns : WAIT_LIMIT_NS;
+    plan->probe_ns = 0;
     cudaError_t e;
     if (d.dtype == MOM_F32) e = launch<float, MOM_F32>(a, per, sm_count, stream);
     else if (d.dtype == MOM_BF16) e = launch<__nv_bfloat16, MOM_BF16>(a, per, sm_count, stream);
@@ -795,6 +812,13 @@ mom_status_t mom_moe_device_status(const mom_moe_plan_t *plan, int32_t *code, in
     }
     *code = host[0];
     if (detail) *detail = host[1];
+    return MOM_OK;
+}
+
+mom_status_t mom_moe_probe_wait_timeout(const mom_moe_plan_t *plan, double limit_ms) {
+    if (!plan || !(limit_ms > 0.0) || limit_ms > 1000.0) return MOM_ERR_INVALID_ARG;
+    std::lock_guard<std::mutex> lock(plan->mutex);
+    plan->probe_ns = (unsigned long long)(limit_ms * 1.0e6) + 1;
     return MOM_OK;
 }
 

@@ -264,3 +264,33 @@ def test_moe_special_tokens_keep_the_others_bits(tokens, dtype):
         y = layer(special)
         others = [i for i in range(tokens) if i != at]
         assert torch.equal(y[others], y0[others]) and y[at].isnan().all()
+
+
+@pytest.mark.parametrize("hidden,inner,count,top_k", [(256, 64, 4, 2), (48, 2000, 9, 3)], ids=["whole rows of D", "rows of D shared by CTAs"])
+def test_moe_wait_that_runs_out(hidden, inner, count, top_k):
+    """The self-test's missing arrival: y is NaN and never a number that may be wrong, the status tells of it once, and the next execute has its bits again."""
+    torch.manual_seed(inner)
+    rng = np.random.default_rng(inner)
+    boxes = [pack(*weights(rng, count, *shape, 32, "bf16", False), 32)[1] for shape in ((inner, hidden), (inner, hidden), (hidden, inner))]
+    x, r = torch.randn(40, hidden, device="cuda").to(torch.bfloat16), torch.randn(count, hidden, device="cuda").to(torch.bfloat16)
+    plan = mom.mom_moe_plan(hidden, inner, count, top_k, mom.BF16, mom.BF16, 32)
+    room = plan.workspace_bytes(40)
+    ws = torch.empty(room, dtype=torch.uint8, device="cuda")
+
+    def layer():
+        y = torch.zeros_like(x)
+        plan.execute(40, ptr(x), ptr(r), *map(ptr, boxes), ptr(y), None, None, ptr(ws), room, stream())
+        torch.cuda.synchronize()
+        return y
+    want = layer()
+    assert plan.device_status() == (0, 0) and want.isfinite().all()
+    plan.probe_wait_timeout(3.0)
+    assert layer().isnan().all()
+    assert torch.equal(layer(), want)                        # also before the status has been read
+    code, detail = plan.device_status()
+    assert code == mom.ERR_DEVICE_TIMEOUT and detail in (1, 2, 3)
+    assert plan.device_status() == (0, 0)
+    assert torch.equal(layer(), want) and plan.device_status() == (0, 0)
+    for bad in (0.0, -1.0, 1001.0):
+        with pytest.raises(mom.MomError):
+            plan.probe_wait_timeout(bad)
