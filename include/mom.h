@@ -554,8 +554,7 @@ typedef struct {
  *   add       T, or NULL; may be y itself (same stride)
  * Made for few tokens (one to a few hundred), where the bytes of W are what costs.  The waits inside the kernel for more than
  * eight tokens are bounded: rows whose wait gave up (which takes a defect of the GPU or of this library) are NaN in Y.
- * Errors: INVALID_ARG, DTYPE, LIMIT (tokens above 2^20, tokens * rows about 2^38), ALIGNMENT (container not 256-byte aligned, another pointer not aligned to its
- * element), ARCH, CUDA. */
+ * Errors: INVALID_ARG, DTYPE, LIMIT (tokens above 2^20), ALIGNMENT (container not 256-byte aligned, another pointer not aligned to its element), ARCH, CUDA. */
 mom_status_t mom_w4_product(const mom_w4_product_desc_t *desc, const void *container, const void *x, const float *x_scales,
                             const void *add, void *y, mom_stream_t stream);
 
