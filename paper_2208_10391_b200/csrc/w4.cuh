@@ -435,11 +435,12 @@ __device__ __forceinline__ void multiply_tile(const W4View &w, const SlotLayout 
             o1.set((z >> 8) & 15u);
         }
         const float2 scale = slot_scales(slot + 2 * W4_TILE_BYTES + (side + group) * l.scale_bytes, g, w.scale_dtype);
-        constexpr int CHAINS = PER > 1 ? 2 : 1;                // of dependent MMAs
+        // Chains of dependent MMAs: the leading term, and the rest on its own, which would else be cut against sums 2^8 times as large (f32
+        // products 1.8e-7 to 2.7e-7 off, apart 0.8e-7); with one term every other stretch.
+        constexpr int CHAINS = PER > 1 || TERMS > 1 ? 2 : 1;
         float acc[CHAINS][4];
 #pragma unroll
         for (int q = q0; q < q0 + PER; ++q) {
-            const int chain = (q - q0) % CHAINS;
             const uint4 v = c[q >> 1];
             uint32_t a[4], b[4];
             unpack_codes<BF16>(q & 1 ? v.z : v.x, o0, a);
@@ -447,7 +448,8 @@ __device__ __forceinline__ void multiply_tile(const W4View &w, const SlotLayout 
 #pragma unroll
             for (int i = 0; i < TERMS; ++i) {
                 const uint4 e = x.get(q, i);
-                if (i == 0 && q - q0 < CHAINS) mma16816_first<BF16>(acc[chain], a[0], b[0], a[1], b[1], e.x, e.y);
+                const int chain = TERMS > 1 ? i > 0 : (q - q0) % CHAINS;
+                if (TERMS > 1 ? q == q0 && i < 2 : q - q0 < CHAINS) mma16816_first<BF16>(acc[chain], a[0], b[0], a[1], b[1], e.x, e.y);
                 else mma16816<BF16>(acc[chain], a[0], b[0], a[1], b[1], e.x, e.y);
                 mma16816<BF16>(acc[chain], a[2], b[2], a[3], b[3], e.z, e.w);
             }

@@ -294,3 +294,37 @@ def test_moe_wait_that_runs_out(hidden, inner, count, top_k):
     for bad in (0.0, -1.0, 1001.0):
         with pytest.raises(mom.MomError):
             plan.probe_wait_timeout(bad)
+
+
+def normwise(got, want):
+    return np.linalg.norm(host(got) - want) / np.linalg.norm(want)
+
+
+@pytest.mark.parametrize("tokens,rows,cols,group,zeros", [(1, 512, 4096, 128, False), (8, 300, 2048, 32, False), (7, 400, 5003, 64, True), (3, 200, 9000, 0, False)])
+def test_w4_product_f32_is_right_to_the_last_unit(tokens, rows, cols, group, zeros):
+    """Normal values, up to eight tokens: normwise off by at most one unit of f32, 2^-23."""
+    torch.manual_seed(cols)
+    codes, s, z = weights(np.random.default_rng(cols), 1, rows, cols, group, "f32", zeros)
+    d, box = pack(codes, s, z, group)
+    x, y = torch.randn(tokens, cols, device="cuda"), torch.empty(tokens, rows, device="cuda")
+    mom.mom_w4_product(mom.mom_w4_product_desc(d, tokens, mom.F32, mom.F32), ptr(box), ptr(x), None, None, ptr(y), stream())
+    torch.cuda.synchronize()
+    assert normwise(y, ref.product(host(x), dense(codes, s, z, group)[0])) <= 2.0 ** -23
+
+
+@pytest.mark.parametrize("tokens,hidden,inner,count,top_k,group", [(5, 1001, 333, 10, 3, 32), (20, 320, 558, 16, 3, 64), (9, 1024, 512, 8, 2, 128)])
+def test_moe_f32_is_right_to_the_last_units(tokens, hidden, inner, count, top_k, group):
+    """Three such products in a row: at most three units."""
+    torch.manual_seed(hidden)
+    rng = np.random.default_rng(hidden)
+    parts = [weights(rng, count, *shape, group, "f32", False) for shape in ((inner, hidden), (inner, hidden), (hidden, inner))]
+    boxes = [pack(*p, group)[1] for p in parts]
+    x, r = torch.randn(tokens, hidden, device="cuda"), torch.randn(count, hidden, device="cuda") / hidden ** 0.5
+    want, ids, _, _, _, gap = ref.moe(host(x), host(r), *(dense(*p, group) for p in parts), top_k, True)
+    plan = mom.mom_moe_plan(hidden, inner, count, top_k, mom.F32, mom.F32, group, mom.F32)
+    room = plan.workspace_bytes(tokens)
+    ws, y = torch.empty(room, dtype=torch.uint8, device="cuda"), torch.empty_like(x)
+    plan.execute(tokens, ptr(x), ptr(r), *map(ptr, boxes), ptr(y), None, None, ptr(ws), room, stream())
+    torch.cuda.synchronize()
+    assert plan.device_status() == (0, 0) and gap > 1e-5
+    assert normwise(y, want) <= 3 * 2.0 ** -23
