@@ -377,13 +377,15 @@ __global__ void __launch_bounds__(THREADS, 1) w4_product_tc_kernel(const W4Produ
                 if (n >= 2 && !(fine = wait_barrier(d_empty + 8 * d, ((n >> 1) - 1) & 1, abort_flag, status, 6))) break;
                 ptx::tc_fence_after_sync();
                 if (elect_one()) {
+                    // (f32 tokens: the small terms of all columns first, so that their sums are not cut against those of the leading one)
 #pragma unroll
-                    for (int q = 0; q < 2 * PER; ++q) {        // 16 columns each
-                        const int k = f * 2 * PER + q;
+                    for (int t = Op::TERMS - 1; t >= 0; --t)
 #pragma unroll
-                        for (int t = 0; t < Op::TERMS; ++t)
-                            mma_f16_a_tmem(tmem + d * D_COLS, a_at + k * 8, desc + ((t * 2 + (k >> 2)) * C::PANEL + (k & 3) * 32) / 16, idesc, q > 0 || t > 0);
-                    }
+                        for (int q = 0; q < 2 * PER; ++q) {    // 16 columns each
+                            const int k = f * 2 * PER + q;
+                            mma_f16_a_tmem(tmem + d * D_COLS, a_at + k * 8, desc + ((t * 2 + (k >> 2)) * C::PANEL + (k & 3) * 32) / 16, idesc,
+                                           q > 0 || t < Op::TERMS - 1);
+                        }
                     ptx::mma_commit(d_full + 8 * d);
                     if (f == FLUSHES - 1) {
                         ptx::mma_commit(a_empty + 8 * sa);

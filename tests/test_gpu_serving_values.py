@@ -328,3 +328,15 @@ def test_moe_f32_is_right_to_the_last_units(tokens, hidden, inner, count, top_k,
     torch.cuda.synchronize()
     assert plan.device_status() == (0, 0) and gap > 1e-5
     assert normwise(y, want) <= 3 * 2.0 ** -23
+
+
+@pytest.mark.parametrize("tokens,rows,cols,group", [(64, 512, 4096, 128), (40, 300, 8192, 0), (20, 700, 5003, 64)])
+def test_w4_product_of_many_f32_tokens_is_right_to_two_units(tokens, rows, cols, group):
+    """Normal values, more than eight tokens (one accumulator for all terms): normwise off by at most two units of f32, 2^-22."""
+    torch.manual_seed(cols)
+    codes, s, z = weights(np.random.default_rng(cols), 1, rows, cols, group, "f32", False)
+    d, box = pack(codes, s, z, group)
+    x, y = torch.randn(tokens, cols, device="cuda"), torch.empty(tokens, rows, device="cuda")
+    mom.mom_w4_product(mom.mom_w4_product_desc(d, tokens, mom.F32, mom.F32), ptr(box), ptr(x), None, None, ptr(y), stream())
+    torch.cuda.synchronize()
+    assert normwise(y, ref.product(host(x), dense(codes, s, z, group)[0])) <= 2.0 ** -22
