@@ -172,8 +172,10 @@ __device__ __forceinline__ float row_max(float v, float *slots) {
     return v;
 }
 
-template <typename T, bool WIDE, bool CODES, int CHUNKS, bool WARP>          // WARP: a warp per row
-__global__ void __launch_bounds__(1024) rms_norm_kernel(NormArgs a) {
+// WARP: a warp per row.  With one chunk, and with two of 16-bit rows without codes, 32 registers, so that CTAs of every size fill an SM
+// (2048 x 4099 to e4m3 27.2 us with 40, 23.8 with 32; 2000 x 12288 in bf16 42.7 with 45, 33.3 with 32).
+template <typename T, bool WIDE, bool CODES, int CHUNKS, bool WARP>
+__global__ void __launch_bounds__(1024, !WARP && (CHUNKS == 1 || (CHUNKS == 2 && !CODES && sizeof(T) == 2)) ? 2 : 1) rms_norm_kernel(NormArgs a) {
     __shared__ float sums[64], largest[32];
     const int lane = threadIdx.x & 31, warp = WARP ? 0 : threadIdx.x >> 5;
     const long long row = WARP ? (long long)blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5) : blockIdx.x;
@@ -182,12 +184,13 @@ __global__ void __launch_bounds__(1024) rms_norm_kernel(NormArgs a) {
     const T *res = a.residual ? static_cast<const T *>(a.residual) + row * a.residual_stride : nullptr;
     T *res_out = a.residual_out ? static_cast<T *>(a.residual_out) + row * a.residual_stride : nullptr;
 
-    // Column of entry j of chunk c: a warp has 256 neighbouring ones of a chunk.  Four chunks: those that two neighbouring warps have with two
-    // chunks, so that every sum has the same bits.
+    // Column of entry j of chunk c: a warp has 256 neighbouring ones of a chunk.  Four chunks of a wide row: those that two neighbouring warps have
+    // with two chunks, so that every sum has the same bits.
+    constexpr bool PAIRED = WIDE && CHUNKS == 4;
     const int half = (a.cols + 511) / 512;
     auto column = [&](int c, int j) {
         const int k = WIDE ? lane * 8 + j : j * 32 + lane;
-        if (CHUNKS == 4) return 2 * warp * 256 + k + (c & 1) * half * 256 + (c >> 1) * (2 * warp + 1 < half ? 256 : a.cols);
+        if (PAIRED) return 2 * warp * 256 + k + (c & 1) * half * 256 + (c >> 1) * (2 * warp + 1 < half ? 256 : a.cols);
         return (WARP ? c : c * (int)(blockDim.x >> 5) + warp) * 256 + k;
     };
 
@@ -234,11 +237,11 @@ __global__ void __launch_bounds__(1024) rms_norm_kernel(NormArgs a) {
                     if (k + 32 * j < a.cols) res_out[k + 32 * j] = from_float<T>(h[c][j]);
             }
         }
-        float &s = c < 2 ? sum : second;
+        float &s = PAIRED && c >= 2 ? second : sum;
 #pragma unroll
         for (int j = 0; j < 8; ++j) s = fmaf(h[c][j], h[c][j], s);
     }
-    const float factor = 1.0f / sqrtf(row_sum<(CHUNKS > 2), WARP>(sum, second, sums) / (float)a.cols + a.eps);
+    const float factor = 1.0f / sqrtf(row_sum<PAIRED, WARP>(sum, second, sums) / (float)a.cols + a.eps);
 
     allow_dependents();
     // y = h * factor * weight
@@ -261,9 +264,15 @@ __global__ void __launch_bounds__(1024) rms_norm_kernel(NormArgs a) {
         }
         // (8 bits: entries beyond the last column stay 0; an infinite factor or weight would make a NaN of them, which the scale would take up)
         const float f = CODES && WIDE && k >= a.cols ? 0.0f : factor;
+        const bool part = CODES && !WIDE && k - lane + 256 > a.cols;         // (of the warp's 256 columns some are beyond the last)
+        if (!part) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-            if (!CODES || WIDE || k + 32 * j < a.cols) h[c][j] = h[c][j] * f * w[j];
+            for (int j = 0; j < 8; ++j) h[c][j] = h[c][j] * f * w[j];
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (k + 32 * j < a.cols) h[c][j] = h[c][j] * factor * w[j];
+        }
     }
 
     if (!CODES) {
@@ -320,24 +329,16 @@ __global__ void __launch_bounds__(1024) rms_norm_kernel(NormArgs a) {
             Divisor(scale).of(h[c], v);
         } else {
             const int per = a.group / 32;                // 1, 2 or 4 columns of the lane share a scale
-            float m[8];
-#pragma unroll
-            for (int j = 0; j < 8; ++j) m[j] = fabsf(h[c][j]);
-            if (per >= 2) {
-#pragma unroll
-                for (int j = 0; j < 8; j += 2) m[j] = m[j + 1] = max_nan(m[j], m[j + 1]);
-            }
-            if (per == 4) {
-#pragma unroll
-                for (int j = 0; j < 8; j += 4) m[j] = m[j + 1] = m[j + 2] = m[j + 3] = max_nan(m[j], m[j + 2]);
-            }
             Divisor by(0.0f);
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 if ((j & (per - 1)) == 0) {
+                    float m = fabsf(h[c][j]);
+                    if (j % 2 == 0 && per >= 2) m = max_nan(m, fabsf(h[c][j + 1]));
+                    if (j % 4 == 0 && per == 4) m = max_nan(m, max_nan(fabsf(h[c][j + 2]), fabsf(h[c][j + 3])));
 #pragma unroll
-                    for (int o = 16; o; o >>= 1) m[j] = max_nan(m[j], __shfl_xor_sync(~0u, m[j], o));
-                    const float scale = scale_of(m[j]);
+                    for (int o = 16; o; o >>= 1) m = max_nan(m, __shfl_xor_sync(~0u, m, o));
+                    const float scale = scale_of(m);
                     const int first = k - lane + 32 * j;
                     if (lane == 0 && first < a.cols) scales[first / a.group] = scale;
                     by = Divisor(scale);
@@ -361,17 +362,18 @@ cudaError_t launch(NormArgs a, int64_t rows, int sm_count, cudaStream_t stream) 
     // Few rows: a thread holds 8 entries (one chain of latencies, as many threads as it takes).  Many rows of up to 512 columns: a warp
     // each, so that CTAs are not the cost (8000 x 320 in bf16 10.1 -> 4.8 us; from 1024 columns on a CTA per row is as good or better).
     // Many longer rows: f32 or narrow one chunk (us with 1 / 2 / 4 chunks: 809 x 6728 in f32 17.7 / 18.8 / 22.2, 2048 x 4099 19.6 / 21.6 / 48).
-    // 16 bits two, and four with 8-bit outputs (64 registers a thread, 32 warps on an SM, where two chunks take 40 and leave 48) if an SM then holds
-    // at least a quarter more rows at once.  Rows of 32 M entries in all, us with 2 / 4 chunks: to e4m3, a scale per 128, 2304 columns
-    // 49.1 / 55.0, 3328 50.2 / 51.9, 4096 47.0 / 46.5, 5120 50.1 / 48.2, 6656 51.9 / 52.2, 7424 50.9 / 50.5, 8192 49.1 / 48.1, 9216 55.3 / 51.8,
-    // 10496 54.2 / 60.8, 12288 51.6 / 55.3, 12544 75.0 / 55.9, 16384 66.6 / 51.1; a scale per row 4096 43.0 / 41.2, 7424 48.0 / 44.6,
-    // 10496 50.7 / 52.6, 16384 62.1 / 45.6.  f16 to f16 2304 41.7 / 43.4, 4096 42.3 / 44.2, 8192 43.1 / 44.8, 12288 44.3 / 44.8, 16384 44.0 / 45.5.
+    // 16 bits two.  With 8-bit outputs four if an SM then holds twice as many rows at once (it has room for 48 warps with the 40 registers a thread
+    // that two chunks take, for 32 with 64), or a quarter more of a call that comes from HBM (2^25 entries are 235 MB).
+    // To e4m3 with a scale per 128, us with 2 / 4 chunks, of 2^24 and 2^26 entries in all: 3328 columns 27.5 / 29.7, 95.6 / 97.3, 4096 26.2 / 27.3,
+    // 94.4 / 90.4, 5120 28.0 / 28.3, 96.5 / 90.2, 6144 27.0 / 28.4, 94.7 / 91.6, 8192 27.4 / 28.4, 97.0 / 90.1, 10240 29.8 / 29.4, 102 / 92,
+    // 12288 29.4 / 32.0, 97 / 102, 12544 40.2 / 32.3, 143 / 104, 16384 36.2 / 29.7, 126 / 93; with a scale per row 4096 24.3 / 24.3, 80.7 / 74.0,
+    // 8192 25.9 / 25.4, 86.1 / 76.6.  f16 to f16, 2^25 entries: 2304 41.7 / 43.4, 4096 42.3 / 44.2, 8192 43.1 / 44.8, 16384 44.0 / 45.5.
     const int pieces = (a.cols + 255) / 256;                          // warps' worth of columns
     const bool codes = !is_float_type(a.out_dtype);
     int chunks = pieces <= 32 ? 1 : pieces <= 64 ? 2 : 4;
     if (rows > 2 * sm_count && WIDE && sizeof(T) == 2 && pieces > 8 && pieces <= 64) {
         const int by_two = 48 / ((pieces + 1) / 2), by_four = 32 / ((pieces + 3) / 4);
-        chunks = codes && 4 * by_four >= 5 * by_two ? 4 : 2;
+        chunks = codes && (by_four >= 2 * by_two || (4 * by_four >= 5 * by_two && rows * a.cols >= 1 << 25)) ? 4 : 2;
     }
     const bool warp_rows = rows > 8 * sm_count && pieces <= 2;
     a.rows = (int)rows;
