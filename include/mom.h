@@ -472,10 +472,10 @@ mom_status_t mom_product_3xtf32_noalloc(int64_t m, int64_t n, int64_t k, mom_pro
 
 /* Root-mean-square norm with the residual's addition, row by row:
  *     h = x + residual;   residual_out = h;   y = h * weight / sqrt(mean(h^2) + eps)
- * y comes in out_dtype.  MOM_F32, MOM_BF16, MOM_F16: the values.  MOM_E4M3, MOM_INT8: per row and group of `group` columns
+ * (f32 throughout, y rounded once).  y comes in out_dtype.  MOM_F32, MOM_BF16, MOM_F16: the values.  MOM_E4M3, MOM_INT8: per row and group of `group` columns
  * (0: the whole row) a scale s = max |y| / Q (Q = 448 resp. 127) and the codes y / s rounded to nearest, ties to even; a
- * group with no |y| of 2^-100 or more has scale 0 and codes 0.  A NaN makes its row's y NaN, an infinity its own y NaN and the row's others 0 (as the
- * formula says); a group that holds a NaN has scale NaN and, in e4m3, NaN codes (int8 has none: 0). */
+ * group with no |y| of 2^-100 or more has scale 0 and codes 0.  The squares are summed in f32: a row whose sum passes f32 (entries of about
+ * 2^63) gives zeros.  A NaN makes its row's y NaN, an infinity its own y NaN and the row's others 0 (as the formula says); a group that holds a NaN has scale NaN and, in e4m3, NaN codes (int8 has none: 0). */
 typedef struct {
     int64_t rows, cols;                              /* rows >= 0, 1 <= cols <= MOM_RMS_NORM_MAX_COLS */
     int64_t x_stride, residual_stride, out_stride;   /* elements between rows, 0: cols; residual_stride holds for residual and residual_out */
@@ -552,8 +552,8 @@ typedef struct {
  * scaled and summed in f32, T is added and the sum rounded once.
  *   x_scales  8-bit X: f32, tokens x ceil(cols / x_group), contiguous (as mom_rms_norm writes them); else NULL
  *   add       T, or NULL; may be y itself (same stride)
- * Made for few tokens (one to a few hundred), where the bytes of W are what costs.  The waits inside the kernel for more than
- * eight tokens are bounded: rows whose wait gave up (which takes a defect of the GPU or of this library) are NaN in Y.
+ * Made for few tokens (one to a few hundred), where the bytes of W are what costs; beyond, W is unpacked again for every 64 tokens.  The waits
+ * inside the kernel for more than eight tokens are bounded: rows whose wait gave up (which takes a defect of the GPU or of this library) are NaN in Y.
  * Errors: INVALID_ARG, DTYPE, LIMIT (tokens above 2^20), ALIGNMENT (container not 256-byte aligned, another pointer not aligned to its element), ARCH, CUDA. */
 mom_status_t mom_w4_product(const mom_w4_product_desc_t *desc, const void *container, const void *x, const float *x_scales,
                             const void *add, void *y, mom_stream_t stream);
@@ -561,6 +561,7 @@ mom_status_t mom_w4_product(const mom_w4_product_desc_t *desc, const void *conta
 /* A mixture-of-experts layer for a few tokens in one launch.  Per token x (hidden entries):
  *     p = softmax(R x);  the top_k largest p_e, equal ones by lowest e;  shares = p_e, divided by their sum if renormalize
  *     y = sum over the chosen e of share_e * D_e (silu(G_e x) * (U_e x)),     silu(v) = v / (1 + exp(-v))
+ * All in f32 (what D_e is applied to included) and y rounded once.  p that are too small for f32 are 0, and equal.
  * R is experts x hidden; G, U (inner x hidden) and D (hidden x inner) are 4-bit containers of `experts` matrices each. */
 typedef struct {
     int64_t hidden, inner;       /* 1 .. MOM_MOE_MAX_WIDTH */

@@ -13,9 +13,10 @@
 //      share * D h over a token's experts in their order: no atomics, the same bits every time.  The first tiles of D are
 //      on their way before the barrier is waited for.  Where D has fewer rows than the GPU has SMs, several CTAs share a row's tiles
 //      and their parts of y are added after a further barrier.
-// Measured: 64 tokens, 64 experts of 4096 x 1280 258 us (520 MB: 2.0 TB/s; the 92 blocks of eight tokens that the experts get are each a pass
-// over the instructions of w4.cuh, which bound it); one token, 64 experts of 2048 x 1024, 24.3 us, a chain of latencies: router 4K cycles,
-// ranking 4K, G and U 15K, D 8K and two barriers; 5 tokens, 10 experts of 1001 x 333 in f32 23.3 us.
+// Measured: 64 tokens, 64 experts of 4096 x 1280 251 us (520 MB: 2.1 TB/s; the 92 blocks of eight tokens that the experts get are each a pass
+// over the instructions of w4.cuh, which bound it), in f32 411 us; one token, 64 experts of 2048 x 1024, 25.5 us, a chain of latencies: router 4K
+// cycles, ranking 4K, G and U 15K, D 8K and two barriers; 5 tokens, 10 experts of 1001 x 333 in f32 23.5 us; 45 tokens, 83 experts of 320 x 558
+// in f32 48 us.
 // Only the chosen experts' weights are read.  Every wait is bounded; a CTA that gives up records it and still arrives at the next barrier, so
 // that nobody waits for it; it writes NaN for its part of y, and so do all that meet it at a later barrier.
 #include <algorithm>
@@ -68,7 +69,7 @@ struct MoeArgs {
     int missing;                   // self-test: arrivals that are waited for and never come
 };
 
-constexpr int H_TERMS = 3;                       // of h as the operand of D (bf16): all 24 bits in layers of every type (two terms, 2^-18 off, took 229 us where three take 258)
+constexpr int H_TERMS = 3;                       // of h as the operand of D (bf16): all 24 bits in layers of every type (64 tokens with two terms, 2^-18 off, 229 us, with three 251)
 
 // Up to eight tokens of one expert.
 struct Block {

@@ -8,7 +8,8 @@
 // is finished by its warp; the (at most two) rows that it shares with its neighbours go to slots that are added in the
 // warps' order once all have arrived, and the cluster's sums are added in its CTAs' order: the same bits every time.
 // Measured: 1 token, 28672 x 8192 bf16 30.5 us (121 MB: 4.0 TB/s of the 6.5 that a copy reaches; 174 warp instructions per tile at 2.65 a
-// cycle bound it, 24 warps or a smaller ring change nothing); 1 x 1024 x 1024 3.5 us (a launch); 7 x 1999 x 5003 in f32 11.7 us.
+// cycle bound it, 24 warps or a smaller ring change nothing); 1 x 1024 x 1024 3.5 us (a launch); 7 x 1999 x 5003 in f32 11.8 us;
+// with 8-bit tokens 1 x 28672 x 8192 30.0 us in e4m3 and in int8, 8 x 28672 x 8192 in e4m3 37 us.
 #include <algorithm>
 
 #include <cooperative_groups.h>

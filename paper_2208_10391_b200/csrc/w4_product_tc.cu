@@ -16,7 +16,9 @@
 // Measured: 64 tokens, 14336 x 4096 f16 26.4 us (285 TFLOP/s, 1.3 TB/s of W), 36 tokens, 6760 x 9024 in e4m3 54 us, 64 tokens, 8192 x 8192 in
 // f32 77 us, 16 tokens, 8192 x 8192 in e4m3 24 us (1.5 TB/s).  29 warps leave 64 registers a thread, and the issue slots that they share bound it,
 // with the flush the slowest role (f32 and 8-bit tokens: the staging).  What a role keeps has to be declared inside it: sums of the flush
-// that lived through all roles spilled 450 to 1900 bytes a thread (29.3, 104 and 219 us).
+// that lived through all roles spilled 450 to 1900 bytes a thread (29.3, 104 and 219 us; 4 to 32 bytes are left with 64 tokens, and with 32 in f32).
+// Prompts: W is unpacked again for every 64 tokens.  4096 x 4096 in bf16 65 tokens 17.7 us, 128 17.2, 256 23.7, 512 46, 1024 92 us (373 TFLOP/s); in
+// e4m3 64 tokens 20 us, 1024 177 us.
 // Every wait is bounded; a CTA in which one gives up ends by itself and writes NaN.
 #include <algorithm>
 
